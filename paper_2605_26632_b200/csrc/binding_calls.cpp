@@ -10,9 +10,11 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/Context.h>
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/core/TensorBody.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <ATen/ops/empty.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -65,8 +67,11 @@ template <class T>
 T* ptr_as(const at::Tensor* t) { return static_cast<T*>(ptr(t)); }
 int64_t ld(const at::Tensor* t) { return t ? t->stride(0) : 0; }
 void* stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
-// (what at::empty comes to on a CUDA device, without the dispatcher's way there: a call that makes two tensors 5.1 -> 4.6 us)
+// (What at::empty comes to on a CUDA device, without the dispatcher's way there: a call that makes two tensors 5.1 -> 4.6 us.  In
+// torch's deterministic mode at::empty also fills the new memory, which rows of no group show.)
 at::Tensor empty(at::IntArrayRef shape, const at::Tensor& like, at::ScalarType type = at::kBFloat16) {
+    if (C10_UNLIKELY(at::globalContext().deterministicAlgorithms() && at::globalContext().deterministicFillUninitializedMemory()))
+        return at::empty(shape, at::TensorOptions().dtype(type).device(like.device()));
     return at::Tensor(at::detail::empty_cuda(shape, type, like.device(), std::nullopt));
 }
 
