@@ -25,6 +25,9 @@
  *     handled inside the kernels.
  *   - A context belongs to one device, and that device must be the calling thread's current
  *     device (cudaSetDevice) whenever the context is used; lynx_create makes it current.
+ *   - The calls that use the context's scratch (all but the MXFP4 and grouped ones) of one context are made by one host thread
+ *     at a time and on one stream at a time.  The MXFP4 and grouped calls use none: they may be made from several host threads and on
+ *     several streams at once, beside one another and beside those.
  *   - There is no CPU fallback: on a device that is not sm_100 lynx_create fails with
  *     LYNX_ERR_UNSUPPORTED_ARCH.
  */

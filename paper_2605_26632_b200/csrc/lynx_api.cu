@@ -8,6 +8,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <atomic>
 #include <mutex>
 
 #include "prune_compress.cuh"
@@ -51,7 +52,7 @@ struct lynx_ctx {
     uint32_t* sk_flags = nullptr;
     uint32_t sk_epoch = 0;
     int streamk = 0;  // stream-K tail: off by default (measured: no net gain), LYNX_STREAMK=1 enables
-    int64_t launches = 0;
+    std::atomic<int64_t> launches{0};  // (MXFP4 and grouped calls may come from several host threads)
     int pdl = 1;        // programmatic dependent launch of the finalize and GEMM kernels
     int gemm_cfg = 0;   // 0 = auto
     int prune_tpu = 0;  // 0 = auto
@@ -152,7 +153,7 @@ bool make_tmap_2d(lynx_ctx* ctx, CUtensorMap* m, CUtensorMapDataType dt, int ele
 // cudaFuncSetAttribute is per device: remember, per kernel instantiation, which devices have it.
 constexpr int MAX_CTX_DEVICES = 64;
 template <class Kernel>
-lynx_status allow_dynamic_smem(Kernel kern, int bytes, int device, bool (&done)[MAX_CTX_DEVICES]) {
+lynx_status allow_dynamic_smem(Kernel kern, int bytes, int device, std::atomic<bool> (&done)[MAX_CTX_DEVICES]) {
     if (device < 0 || device >= MAX_CTX_DEVICES) return LYNX_ERR_INVALID_ARG;
     if (done[device]) return LYNX_OK;
     if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess)
@@ -163,7 +164,7 @@ lynx_status allow_dynamic_smem(Kernel kern, int bytes, int device, bool (&done)[
 
 // The same for the kernels that move registers between their warpgroups.
 template <class Kernel>
-lynx_status prepare_gemm_kernel(Kernel kern, int bytes, int device, bool (&done)[MAX_CTX_DEVICES]) {
+lynx_status prepare_gemm_kernel(Kernel kern, int bytes, int device, std::atomic<bool> (&done)[MAX_CTX_DEVICES]) {
     if (device >= 0 && device < MAX_CTX_DEVICES && !done[device]) {
         cudaFuncAttributes fa;
         if (cudaFuncGetAttributes(&fa, kern) != cudaSuccess || !gemm_register_shares_fit(fa.numRegs)) return LYNX_ERR_CUDA;
@@ -433,7 +434,7 @@ lynx_status launch_gemm_cfg(lynx_ctx* ctx, const void* values, const void* meta,
     p.trigger = p.w_prefetch;  // read by the low-rank kernels: their layers' prune launch has a block per SM
 
     auto kern = lora ? sparse_gemm_kernel<Cfg, true> : sparse_gemm_kernel<Cfg, false>;
-    static bool attr_set[2][MAX_CTX_DEVICES] = {};  // per instantiation (with / without the low-rank code)
+    static std::atomic<bool> attr_set[2][MAX_CTX_DEVICES] = {};  // per instantiation (with / without the low-rank code)
     if (lynx_status as = prepare_gemm_kernel(kern, Cfg::SMEM_BYTES, ctx->device, attr_set[lora ? 1 : 0]); as != LYNX_OK)
         return as;
     const int tiles = p.tiles_m * p.tiles_n;
@@ -606,7 +607,7 @@ lynx_status launch_gemm_rt2(lynx_ctx* ctx, const Rt2Plan& plan, const void* valu
     set_gemm_params(p, ctx, M, N, K, wscale, bias, comp, ss, LORA ? lora->R / 64 : 0, layer_call);
     p.sched.init((int)((M + 255) / 256), (int)((N + Cfg::BN - 1) / Cfg::BN), plan.clusters, plan.doubles, 8);
     auto kern = sparse_gemm_rt2_kernel<Cfg, LORA>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = prepare_gemm_kernel(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(plan.clusters * 2));
@@ -685,7 +686,7 @@ lynx_status launch_gemm_split(lynx_ctx* ctx, int splits, bool next_early, const 
     p.splits = splits;
     const int tiles_n = (int)((N + Cfg::BN - 1) / Cfg::BN);
     auto kern = sparse_gemm_split_kernel<Cfg, LORA>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = prepare_gemm_kernel(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     cudaLaunchConfig_t cfg = {};
     const int grid = p.tiles_m * tiles_n * splits * Cfg::CG;
@@ -879,7 +880,7 @@ lynx_status launch_gemm_fp8_cfg(lynx_ctx* ctx, const void* values_q, const void*
     p.w_prefetch = layer_call ? 1 : 0;
     p.trigger = layer_call && ctx->fp8_ring && fp8_ring_slots(K) ? 1 : 0;
     auto kern = sparse_gemm_kernel<Cfg, false>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = prepare_gemm_kernel(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     const int tiles = p.tiles_m * p.tiles_n;
     int clusters = ctx->num_sms / Cfg::CG;
@@ -954,7 +955,7 @@ lynx_status launch_fused(lynx_ctx* ctx, const void* X, int64_t M, int64_t K, int
     p.dev_error = ctx->err_dev;
     p.tiles_m = (int)((M + Cfg::BM - 1) / Cfg::BM);
     p.tiles_n = (int)((N + Cfg::BN - 1) / Cfg::BN);
-    static bool attr_set[MAX_CTX_DEVICES] = {};
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};
     if (lynx_status as = allow_dynamic_smem(fused_linear_kernel, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK)
         return as;
     int grid = p.tiles_m * p.tiles_n;
@@ -1080,7 +1081,7 @@ lynx_status launch_lora_down(lynx_ctx* ctx, const void* X, int64_t M, int64_t K,
     p.tickets = ctx->tickets + PRUNE_TICKET_BYTES / 4;
     p.dev_error = ctx->err_dev;
     auto kern = lora_down_kernel<Cfg>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = allow_dynamic_smem(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     const int tiles_m = (int)((M + Cfg::BM - 1) / Cfg::BM);
     cudaLaunchConfig_t cfg = {};
@@ -1139,7 +1140,7 @@ lynx_status launch_prune_lora(lynx_ctx* ctx, const void* X, int64_t M, int64_t K
                       (uint64_t)ldlb * 2, 64, Cfg::R, CU_TENSOR_MAP_SWIZZLE_128B))
         return LYNX_ERR_CUDA;
     auto kern = prune_lora_kernel<Cfg, SUMS>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = allow_dynamic_smem(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     PruneLoraParams p;
     p.M = M; p.K = K;
@@ -1297,7 +1298,7 @@ lynx_status launch_grouped_cfg(lynx_ctx* ctx, const GroupedArgs& a, cudaStream_t
                            p.cuts, p.items);
     }
     auto kern = grouped_gemm_kernel<Cfg>;
-    static bool attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
+    static std::atomic<bool> attr_set[MAX_CTX_DEVICES] = {};  // per instantiation
     if (lynx_status as = allow_dynamic_smem(kern, Cfg::SMEM_BYTES, ctx->device, attr_set); as != LYNX_OK) return as;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(clusters * Cfg::CG));
@@ -1542,7 +1543,7 @@ lynx_status lynx_reserve(lynx_ctx* ctx, int64_t M, int64_t N, int64_t K) {
     return ensure_scratch(ctx, scratch_layout(M, K).total);
 }
 
-int64_t lynx_launch_count(lynx_ctx* ctx) { return ctx ? ctx->launches : -1; }
+int64_t lynx_launch_count(lynx_ctx* ctx) { return ctx ? ctx->launches.load(std::memory_order_relaxed) : -1; }
 
 // The prune/compress launch.  defer (ROW mode only): the kernel stops at the per-K-split row sums
 // and `src` tells the following GEMM where they are; its epilogue adds them in the same order the
@@ -2102,7 +2103,7 @@ lynx_status lynx_prune_compress_fp8(lynx_ctx* ctx, const void* X, int64_t M, int
         static const RingKernel kerns[16] = {LYNX_RING4(false, false), LYNX_RING4(true, false),
                                              LYNX_RING4(false, true), LYNX_RING4(true, true)};
 #undef LYNX_RING4
-        static bool attr_set[16][MAX_CTX_DEVICES] = {};
+        static std::atomic<bool> attr_set[16][MAX_CTX_DEVICES] = {};
         const int which = (sums ? 4 : 0) + (given ? 8 : 0) + (gw == 1 ? 0 : gw == 2 ? 1 : gw == 4 ? 2 : 3);
         if (lynx_status as = allow_dynamic_smem(kerns[which], FP8_RING_SMEM_MAX, ctx->device, attr_set[which]);
             as != LYNX_OK)

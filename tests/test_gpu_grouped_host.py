@@ -1,4 +1,6 @@
-"""The host's side of the MXFP4 and grouped calls."""
+"""The host's side of the MXFP4 and grouped calls: what the compiled calls allocate, and the context's state under several threads."""
+import threading
+
 import pytest
 import torch
 
@@ -42,3 +44,32 @@ def test_new_results_are_filled_in_the_deterministic_mode(pair):
                 assert filled(t[none]).all() and not filled(t[10:200]).all()
     finally:
         torch.use_deterministic_algorithms(False)
+
+
+def test_launches_of_two_threads_are_all_counted(pair):
+    """One context, two threads with a stream and tensors each, through the C ABI: calls as close to one another as they come.  (A plain
+    counter lost 3 of 200000.)"""
+    lx, calls = pair[0], 400000
+    sets = []
+    for i in range(2):
+        X = rand((1, 32), 10 + i).cuda()
+        sets.append((X, *lx.quantize_mxfp4(X), torch.cuda.Stream()))
+    want = [s[1].clone() for s in sets]
+    torch.cuda.synchronize()
+    before, start, status = lx.launch_count(), threading.Barrier(2), []
+
+    def work(X, codes, scales, stream):
+        torch.cuda.set_device(0)
+        f = lx._lib.lynx_quantize_mxfp4
+        a = [t(v) for t, v in zip(f.argtypes, (lx._address, X.data_ptr(), 1, 32, 32, None, 1, codes.data_ptr(), scales.data_ptr(), stream.cuda_stream))]
+        start.wait()
+        status.append(sum(f(*a) for _ in range(calls)))
+
+    threads = [threading.Thread(target=work, args=s) for s in sets]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert status == [0, 0] and all(torch.equal(s[1], w) for s, w in zip(sets, want))
+    assert lx.launch_count() - before == 2 * calls
