@@ -48,7 +48,6 @@ struct GroupedParams {
     int groups;
     int tiles_w;        // row tiles of W per group
     int w_blocks;       // 128-row scale tiles of W per group (MXFP4)
-    int chunks;         // scale tiles along K (MXFP4)
     int k_steps;        // MMAs along K
     const float* row_scale;    // [M] or nullptr
     const uint16_t* bias;      // [groups x N] or nullptr

@@ -1239,7 +1239,6 @@ lynx_status launch_grouped_cfg(lynx_ctx* ctx, const GroupedArgs& a, cudaStream_t
     p.groups = a.groups;
     p.tiles_w = (int)((a.N + Cfg::W_ROWS - 1) / Cfg::W_ROWS);
     p.w_blocks = (int)w_blocks;
-    p.chunks = (int)chunks;
     p.k_steps = (int)((a.K + Cfg::STEP_K - 1) / Cfg::STEP_K);
     p.row_scale = a.comp ? a.comp->row_scale : nullptr;
     p.bias = static_cast<const uint16_t*>(a.bias);
@@ -1283,8 +1282,7 @@ lynx_status launch_grouped_cfg(lynx_ctx* ctx, const GroupedArgs& a, cudaStream_t
             if (quarters > 4 * ((tiles + clusters - 1) / clusters)) cluster = 1;
         }
         if (ctx->cluster_cap[cluster] < clusters) clusters = ctx->cluster_cap[cluster];
-        const int64_t most = (tiles * cluster + cluster - 1) / cluster * cluster;
-        if (clusters > most) clusters = most;
+        if (clusters > tiles * cluster) clusters = tiles * cluster;
         clusters = clusters / cluster * cluster;
         p.cluster = cluster;
     } else if (clusters > token_tiles * p.tiles_w * Cfg::MAX_CUTS) {

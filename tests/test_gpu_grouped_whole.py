@@ -167,3 +167,19 @@ def test_tiles_of_either_width_give_the_same_bits(contexts, M, K):
     if K <= 704:
         Y = [lx.grouped_linear(X, off, torch.stack([W, W])) for lx in contexts]
         assert torch.equal(Y[0], Y[1]) and torch.equal(Y[1], Y[2])
+
+
+@pytest.mark.parametrize("M,K", [(1, 3840), (4, 3840), (40, 3840), (150, 3840), (150, 320)])
+def test_result_over_its_residual(contexts, M, K):
+    """In place, where K is split and where it is not, in one launch and in two."""
+    N = 392
+    X, W, res = rand((M, K), 460).cuda(), rand((2 * N, K), 461, K ** -0.5).cuda(), rand((M, N), 462).cuda()
+    off = torch.tensor([0, M // 2, M], dtype=torch.int32, device="cuda")
+    for lx in contexts:
+        wq, ws = lx.quantize_mxfp4(W, groups=2)
+        one, one_s = lx.quantize_mxfp4(W[:N])
+        for call in (lambda **kw: lx.act_linear_mxfp4(X, one, one_s, **kw), lambda **kw: lx.grouped_linear(X, off, W.view(2, N, K), **kw),
+                     lambda **kw: lx.act_grouped_linear_mxfp4(X, off, wq.view(2, N, K // 2), ws, **kw)):
+            over = res.clone()
+            assert call(residual=over, out=over) is over
+            assert torch.equal(over, call(residual=res))
