@@ -356,6 +356,8 @@ LYNX_API lynx_status lynx_act_sparse_linear_fp8(lynx_ctx* ctx, const void* X, in
  * lynx_dequantize_mxfp4:  the bf16 values that codes and scales stand for (exact; a scale of 255 gives NaN).  X as above.
  * lynx_linear_mxfp4:  Y[m, n] = bf16_rne( r_m * sum_k X[m,k] W[n,k] + bias[n] + Yr[m,n] ), X and W in MXFP4 (W: N rows, one
  *   group), accumulated in fp32 on the block-scaled tensor cores; r_m, Yr: comp->row_scale, comp->residual (optional).
+ *   As in lynx_sparse_linear r_m multiplies the product alone; bias and residual are added as they are, in the grouped products too.  (A
+ *   router's weight on experts with biases, which multiplies the bias as well, belongs where the experts' rows are summed.)
  *   Calls of one shape on one GPU repeat bit for bit; products of few tiles and long rows split K and add their parts in a fixed
  *   order, so a row's last bits may differ between batches of different sizes.
  * lynx_grouped_linear_mxfp4:  the same with W and bias of the row's group: Wq groups * N rows (equal groups, offsets NULL, when

@@ -626,7 +626,7 @@ class Lynx:
 
     def linear_mxfp4(self, codes: torch.Tensor, scales: torch.Tensor, Wq: torch.Tensor, wscales: torch.Tensor, bias=None,
                      row_scale=None, residual=None, out=None) -> torch.Tensor:
-        """row_scale * X W^T + bias + residual, X and W as ``quantize_mxfp4`` gives them."""
+        """row_scale * (X W^T) + bias + residual, X and W as ``quantize_mxfp4`` gives them; the factor of a row is not one of the bias."""
         r = self._calls.mx_linear(self._address, self.device.index, codes, scales, Wq, wscales, bias, row_scale, residual, out)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_linear_mxfp4")
@@ -671,7 +671,8 @@ class Lynx:
 
     def grouped_linear(self, X: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, bias=None, row_scale=None, residual=None,
                        out=None) -> torch.Tensor:
-        """Rows [offsets[g], offsets[g+1]) of X times W[g]^T (bf16, W [E, N, K], bias [E, N]); rows of no group are left as they were."""
+        """Rows [offsets[g], offsets[g+1]) of X times W[g]^T (bf16, W [E, N, K], bias [E, N]); rows of no group are left as they were.
+        ``row_scale`` multiplies the product, not the bias (so a router's weight on experts with biases goes where the rows are summed)."""
         r = self._calls.grouped(self._address, self.device.index, X, offsets, W, bias, row_scale, residual, out)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_grouped_linear")

@@ -183,3 +183,20 @@ def test_result_over_its_residual(contexts, M, K):
             over = res.clone()
             assert call(residual=over, out=over) is over
             assert torch.equal(over, call(residual=res))
+
+
+@pytest.mark.parametrize("M,K", [(2, 3840), (150, 320), (150, 3840)])
+def test_factor_of_a_row_is_for_the_product_only(contexts, M, K):
+    """With a factor of 0 the fp32 sum of bias and residual is left, to the bit."""
+    N = 264
+    X, W, bias, res = rand((M, K), 470).cuda(), rand((2 * N, K), 471).cuda(), rand((2, N), 472).cuda(), rand((M, N), 473).cuda()
+    off, zero = torch.tensor([0, M // 2, M], dtype=torch.int32, device="cuda"), torch.zeros(M, device="cuda")
+    one = (bias[0].double() + res.double()).float().to(torch.bfloat16)
+    two = (bias[(torch.arange(M, device="cuda") >= M // 2).long()].double() + res.double()).float().to(torch.bfloat16)
+    for lx in contexts:
+        wq, ws = lx.quantize_mxfp4(W, groups=2)
+        q, s = lx.quantize_mxfp4(W[:N])
+        assert torch.equal(lx.act_linear_mxfp4(X, q, s, bias[0], res, zero), one)
+        assert torch.equal(lx.linear_mxfp4(*lx.quantize_mxfp4(X), q, s, bias[0], zero, res), one)
+        assert torch.equal(lx.grouped_linear(X, off, W.view(2, N, K), bias, zero, res), two)
+        assert torch.equal(lx.act_grouped_linear_mxfp4(X, off, wq.view(2, N, K // 2), ws, bias, zero, res), two)
