@@ -589,7 +589,11 @@ class Lynx:
     def quantize_mxfp4(self, X: torch.Tensor, offsets=None, groups: int = 1, codes=None, scales=None):
         """-> (codes uint8 [M, K/2], scales uint8, in the order the product reads them).  Rows may be cut into groups, by
         ``offsets`` (int32 [groups + 1] on the device: tokens sorted by expert) or into ``groups`` equal ones (the
-        experts' weight matrices, one below the other)."""
+        experts' weight matrices, one below the other).
+
+        Rows of no group (before the first offset, from the last one on) are not written, here and in every call that takes offsets: in
+        buffers of the caller's they are left as they were, in a tensor that the call makes they are uninitialised.  A program that reads
+        them passes its own."""
         r = self._calls.mx_quantize(self._address, self.device.index, X, offsets, groups, codes, scales)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_quantize_mxfp4")
@@ -609,7 +613,8 @@ class Lynx:
         return codes, scales
 
     def dequantize_mxfp4(self, codes: torch.Tensor, scales: torch.Tensor, offsets=None, groups: int = 1, out=None) -> torch.Tensor:
-        """The bf16 values that ``quantize_mxfp4``'s result stands for: [M, K].  With offsets, rows of no group are left as they were."""
+        """The bf16 values that ``quantize_mxfp4``'s result stands for: [M, K].  With offsets, rows of no group are left as they were in
+        ``out`` (without it: uninitialised)."""
         r = self._calls.mx_dequantize(self._address, self.device.index, codes, scales, offsets, groups, out)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_dequantize_mxfp4")
@@ -671,7 +676,8 @@ class Lynx:
 
     def grouped_linear(self, X: torch.Tensor, offsets: torch.Tensor, W: torch.Tensor, bias=None, row_scale=None, residual=None,
                        out=None) -> torch.Tensor:
-        """Rows [offsets[g], offsets[g+1]) of X times W[g]^T (bf16, W [E, N, K], bias [E, N]); rows of no group are left as they were.
+        """Rows [offsets[g], offsets[g+1]) of X times W[g]^T (bf16, W [E, N, K], bias [E, N]); rows of no group are left as they were
+        in ``out`` (without it: uninitialised).
         ``row_scale`` multiplies the product, not the bias (so a router's weight on experts with biases goes where the rows are summed)."""
         r = self._calls.grouped(self._address, self.device.index, X, offsets, W, bias, row_scale, residual, out)
         if r is not None:
@@ -692,7 +698,8 @@ class Lynx:
 
     def grouped_linear_mxfp4(self, codes: torch.Tensor, scales: torch.Tensor, offsets: torch.Tensor, Wq: torch.Tensor,
                              wscales: torch.Tensor, bias=None, row_scale=None, residual=None, out=None) -> torch.Tensor:
-        """``grouped_linear`` on MXFP4 operands: X quantised with the same offsets, Wq [E, N, K/2] quantised in E equal groups."""
+        """``grouped_linear`` on MXFP4 operands: X quantised with the same offsets, Wq [E, N, K/2] quantised in E equal groups; ``out`` and
+        ``row_scale`` as there."""
         r = self._calls.mx_grouped(self._address, self.device.index, codes, scales, offsets, Wq, wscales, bias, row_scale, residual, out)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_grouped_linear_mxfp4")
@@ -713,7 +720,8 @@ class Lynx:
 
     def act_grouped_linear_mxfp4(self, X: torch.Tensor, offsets: torch.Tensor, Wq: torch.Tensor, wscales: torch.Tensor, bias=None,
                                  row_scale=None, residual=None, out=None) -> torch.Tensor:
-        """The whole grouped layer on bf16 activations: ``quantize_mxfp4`` with the offsets and ``grouped_linear_mxfp4``."""
+        """The whole grouped layer on bf16 activations: ``quantize_mxfp4`` with the offsets and ``grouped_linear_mxfp4``; ``out`` and
+        ``row_scale`` as in ``grouped_linear``."""
         r = self._calls.mx_grouped_layer(self._address, self.device.index, X, offsets, Wq, wscales, bias, row_scale, residual, out)
         if r is not None:
             return r if type(r) is not int else _check(r, "lynx_act_grouped_linear_mxfp4")
