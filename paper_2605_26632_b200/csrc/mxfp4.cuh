@@ -11,7 +11,7 @@
 // (r % 32) * 16 + (r / 32) * 4, and the tiles of a row tile follow one another along k.
 //
 // What bounds both kernels is memory: 2 + 17/32 bytes per element.  A lane takes one block of 32 (64 bytes in flight per thread, 2048
-// threads per SM), four lanes a piece of 128 elements, whose four scales are one 4-byte store; the L2 puts the tiles together.  A
+// threads per SM; dequantising 16 bytes and, with 34 registers, 1536), four lanes a piece of 128 elements, whose four scales are one 4-byte store; the L2 puts the tiles together.  A
 // warp's pieces run on over the rows' ends, or, with offsets, stay in one row, which finds its group itself.  16384 x 10240: 66 us,
 // 6.4 TB/s, the rate of a copy; 16384 x 3840 26.4 us; 77 x 3840 1.6; 64 rows in 64 groups 2.2.  Warps that stay in one row without
 // offsets too: 10927 x 128 4.2 us (now 1.7), 16384 x 1088 10.7 (7.7), 16384 x 1536 11.0 (10.0), the same from K = 3840 on.  Blocks of 128
